@@ -93,9 +93,11 @@ quads_status launch_fp8_front(const uint16_t* x, int64_t rows, int K, uint8_t* c
 // Weight quantizer: one CTA per 128 x 128 tile (256 threads, 64 values each: half a row).
 // codes [n, N, K] u8; exps [n, ceil(N/128), ceil(K/128)] u8; atoms [.., 512] u8: the tile's scale byte
 // repeated, the form the tensor-core path copies into tensor memory.  What a last tile lacks counts as zeros.
+// The kernel in front may still read what stands where these codes go, or write w.
 __global__ void __launch_bounds__(256)
 fp8_quantize_weight_kernel(const uint16_t* __restrict__ w, int N, int K, uint8_t* __restrict__ codes,
                            uint8_t* __restrict__ exps, uint8_t* __restrict__ atoms) {
+  pdl_sync();
   const int kt = (K + 127) >> 7, nt = (N + 127) >> 7;
   const int tile = blockIdx.x % (nt * kt), tensor = blockIdx.x / (nt * kt);
   const int tn = tile / kt, tk = tile - tn * kt;

@@ -349,3 +349,28 @@ def test_few_rows_through_the_whole_contraction_again_and_again(B, T, N, K):
     outs = [B.fp8_linear(xd, q) for _ in range(20)]
     assert all(B.moe_async_status(r["workspace"]) == 0 and torch.equal(r["out"], outs[0]["out"]) for r in outs)
     _near(outs[0]["out"], L.forward(_f32(x), _f32(w)), K, True)
+
+
+def test_weights_quantized_where_the_call_in_front_reads_and_from_what_it_writes(B):
+    """The weights' quantizer may be launched while the kernel in front still runs: it writes and reads behind that one's end."""
+    T, N, K = 8192, 2048, 2048
+    x, ws = _acts(T, K, 1).cuda(), [_weight(N, K, s)[None].cuda() for s in (2, 3)]
+    qs = [B.fp8_quantize_weights(w) for w in ws]
+    want = [B.fp8_linear(x, q)["out"] for q in qs]
+    q = {k: v.clone() for k, v in qs[0].items()}
+    got = []
+    torch.cuda.synchronize()
+    for i in range(1, 21):
+        got.append(B.fp8_linear(x, q)["out"])
+        B.check(B.lib.quads_fp8_quantize_weights(B._ptr(ws[i % 2]), 1, N, K, B._ptr(q["q"]), B._ptr(q["exps"]), B._ptr(q["atoms"]), B._stream()))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        assert torch.equal(out, want[i % 2]), i
+    gs = torch.tensor([0.002]).cuda()
+    fq = B.fake_quant_activations(ws[0][0], gs=gs)[0]
+    torch.cuda.synchronize()
+    want = B.fp8_quantize_weights(fq[None])
+    for _ in range(20):
+        got = B.fp8_quantize_weights(B.fake_quant_activations(ws[0][0], gs=gs)[0][None])
+        assert all(torch.equal(got[k], want[k]) for k in want)
+        del got
