@@ -71,7 +71,8 @@ size_t quads_sf_tiled_bytes(int64_t rows, int64_t K);
  * Inference", paragraph FP4.
  *   x      bf16 [rows, K], row stride `ld` elements (ld >= K, ld % 16 == 0),
  *          32-byte aligned
- *   gs_in  float[1] per-tensor scale, or NULL: amax(x)/2688 computed on device
+ *   gs_in  float[1] per-tensor scale, or NULL: amax(x)/2688 computed on device.  (Here and wherever a scale is given, one below
+ *          zero quantizes as its magnitude does, with the signs of the codes turned, so that the values they stand for are the same.)
  *   q      out, u8 [rows, K/2]
  *   sf     out, u8, layout per `sf_layout` ([rows, K/16] when linear)
  *   gs_out out, float[1]: the per-tensor scale that was used (may be NULL)

@@ -223,7 +223,7 @@ struct QuantCtx {
 
 __device__ __forceinline__ void quant_ctx_scalars(QuantCtx& c, float gs) {
   c.gs = gs;
-  c.d6 = __fmul_rn(6.0f, gs);
+  c.d6 = fabsf(__fmul_rn(6.0f, gs));     // (a scale below zero: block scales by its magnitude, codes below 128, the values' signs turned)
   c.r6 = __frcp_rn(c.d6);
 }
 // Entry `code` of the reciprocal table for per-tensor scale gs.

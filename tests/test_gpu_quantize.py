@@ -274,3 +274,33 @@ def test_a_bounded_wait_that_runs_out_is_reported_and_harmless(B, monkeypatch):
     finally:
         lib.quads_debug_set_quantize_wait(0, 0)
     assert torch.equal(q2, q) and torch.equal(sf2, sf) and g3.item() == gs.item()
+
+
+def test_a_given_scale_below_zero(B):
+    """The block scales are those of its magnitude (a code of theirs below zero would index beyond the table of reciprocals) and the codes
+    have the other sign: every value, score and product is the same."""
+    gs = torch.tensor([0.004]).cuda()
+    for rows, K in ((3, 64), (333, 2048)):
+        x = _bf16((rows, K), 5, 3.0)
+        x[1, 16:32] = 0
+        x = x.cuda()
+        (q, sf, g), (qn, sfn, gn) = B.quantize_nvfp4(x, gs=gs), B.quantize_nvfp4(x, gs=-gs)
+        assert torch.equal(sf, sfn) and gn.item() == -g.item()
+        flip = (sf != 0).repeat_interleave(8, dim=1).to(torch.uint8) * 0x88
+        assert torch.equal(q ^ flip, qn)
+        assert torch.equal(B.fake_quant_activations(x, gs=gs)[0], B.fake_quant_activations(x, gs=-gs)[0])
+    for T, H in ((7, 256), (700, 512)):
+        x, w = _bf16((T, H), 6, 3.0).cuda(), _bf16((1, 256, H), 7, 0.05).cuda()
+        a, b = (B.rac_channel_scores(x, gs=s) for s in (gs, -gs))
+        assert torch.equal(a, b)
+        packed = B.fake_quant_weights(w, want_fq=False, sf_layout=B.SF_TILED)
+        a, b = (B.dense_w4a4_rac(x, packed, 64, a_gs=s)["out"].double() for s in (gs, -gs))
+        # the same terms with two signs turned: 2 H additions of either side off by a step (2^-23) of the magnitudes' sum (an E2M1 value is at most
+        # 5/4 of what it stands for, 3/2 with a block scale rounded up; the residual less than half of x), one rounding to bf16 of either
+        mags = x.double().abs() @ w[0].double().abs().t() * 4
+        assert ((a - b).abs() <= 4 * H * 2.0 ** -23 * mags + 2 * 2.0 ** -8 * a.abs() + 1e-30).all()
+        E, I, k = 8, 128, 2
+        w13, w2 = (B.fake_quant_weights(_bf16(s, 8, 0.05).cuda(), want_fq=False, sf_layout=B.SF_TILED) for s in ((E, 2 * I, H), (E, H, I)))
+        lg = torch.randn(T, E, generator=torch.Generator().manual_seed(9)).cuda()
+        a, b = (B.moe_w4a4_rac(x, lg, w13, w2, k, 64, 32, s, a13_gs=s)["out"].double() for s in (gs, -gs))
+        assert torch.isfinite(a).all() and (a - b).norm() <= 1e-2 * a.norm()       # (values of h next to a border, as against the oracle)
