@@ -319,13 +319,8 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   if (bias && (bias->scalar_type() != at::kFloat || bias->dim() != 1 || bias->size(0) != r.E || !bias->is_contiguous() || !is_here(*bias))) Py_RETURN_NONE;
   r.bias = (const float*)ptr(bias);
-  // one piece of memory for both (0.9 us each), the weights 512 bytes or a multiple behind
-  const int64_t n = (int64_t)r.T * r.topk, behind = (n + 127) / 128 * 128, sizes[2] = {r.T, r.topk};
-  at::Tensor ids = alloc({behind + n}, *lg, at::kInt);
-  at::Tensor w = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(ids.storage()), ids.key_set(), caffe2::TypeMeta::Make<float>());
-  ids.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
-  w.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
-  w.unsafeGetTensorImpl()->set_storage_offset(behind);
+  // (a storage each: one that both types share can't be saved together with the other, and keeps both alive)
+  at::Tensor ids = alloc({r.T, r.topk}, *lg, at::kInt), w = alloc({r.T, r.topk}, *lg, at::kFloat);
   r.topk_ids = (int32_t*)ids.data_ptr();
   r.topk_w = (float*)w.data_ptr();
   void* st = stream();

@@ -1,4 +1,5 @@
 """The router by itself and its gradient against the float64 oracle: chosen ids exactly, weights and gradients to float32 rounding."""
+import io
 import math
 
 import numpy as np
@@ -273,3 +274,19 @@ def test_scores_that_crowd_together(B, scale):
             cpu = {a: (v.double().numpy() if torch.is_tensor(v) else v) for a, v in kw.items()}
             for t in range(0, T, 101):
                 assert ids[t].tolist() == R.choose(l[t].double().numpy(), 6, score, **cpu), (score, t)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_ids_and_weights_are_tensors_of_their_own(B, native, monkeypatch):
+    """They can be saved together, as a rollout's routing is for the trainer, and either alone without the other's memory."""
+    if not native:
+        monkeypatch.setattr(B, "_native", None)
+    for T in (1, 40, 3000):
+        ids, w = B.route_experts(_logits(T, 64, T).cuda(), 5)
+        assert ids.untyped_storage().data_ptr() != w.untyped_storage().data_ptr()
+        assert ids.untyped_storage().nbytes() == w.untyped_storage().nbytes() == T * 5 * 4 and ids.storage_offset() == w.storage_offset() == 0
+        f = io.BytesIO()
+        torch.save((ids, w), f)
+        f.seek(0)
+        a, b = torch.load(f)
+        assert a.dtype == torch.int32 and b.dtype == torch.float32 and torch.equal(a, ids) and torch.equal(b, w)
