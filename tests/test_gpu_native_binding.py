@@ -131,3 +131,59 @@ def test_calls_on_the_current_stream():
         got = B.quantize_nvfp4(x)
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def _calls_that_allocate(B):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    def bf(*shape):
+        return (torch.randn(*shape, device="cuda", generator=g) * 0.5).to(torch.bfloat16)
+    T, H, I, E = 3, 256, 128, 8
+    x, lg, dy = bf(T, H), torch.randn(T, E, device="cuda", generator=g), bf(T, 48)
+    w13, w2 = (B.fake_quant_weights(bf(E, *s), want_fq=False, sf_layout=B.SF_TILED) for s in ((2 * I, H), (H, I)))
+    p13, p2 = (B.fp8_quantize_weights(bf(E, *s)) for s in ((2 * I, H), (H, I)))
+    w, wq, a2 = B.fake_quant_weights(bf(1, 384, H), want_fq=False, sf_layout=B.SF_TILED), B.fp8_quantize_weights(bf(1, 48, H)), torch.tensor([0.01], device="cuda")
+    ids, dw = B.route_experts(lg, 2)
+    return [lambda: B.moe_w4a4_rac(x, lg, w13, w2, 2, 0, 0, a2), lambda: B.moe_fp8_w8a8(x, lg, p13, p2, 2), lambda: B.dense_w4a4_rac(x, w, 0),
+            lambda: B.dense_one_sided(x, B.W4A16, w=w), lambda: B.quantize_nvfp4(x), lambda: B.route_experts(lg, 2),
+            lambda: B.route_experts_backward(lg, ids, dw), lambda: B.fp8_linear(x, wq), lambda: B.fp8_linear_backward(dy, x, wq)]
+
+
+def test_allocations_are_seen_by_those_who_watch(monkeypatch):
+    """Dispatch modes and profilers see the tensors that a native call makes, as they see its Python twin's."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+    from paper_2607_15810_b200 import binding as B
+
+    class Seen(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            r = func(*args, **(kwargs or {}))
+            if func is torch.ops.aten.empty.memory_format:
+                self.made.append((tuple(r.shape), r.dtype))
+            return r
+    calls = _calls_that_allocate(B)
+    for i, call in enumerate(calls):
+        made = []
+        for native in (B._native, None):
+            monkeypatch.setattr(B, "_native", native)
+            with Seen() as mode:
+                mode.made = []
+                call()
+            made.append(sorted(mode.made, key=str))
+        monkeypatch.undo()
+        assert made[0] and made[0] == made[1], i
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CPU]) as prof:
+        B.route_experts_backward(torch.zeros(2, 8, device="cuda"), *B.route_experts(torch.zeros(2, 8, device="cuda"), 2))
+    assert sum(e.count for e in prof.key_averages() if e.key == "aten::empty") >= 3
+
+
+def test_memory_is_filled_where_deterministic_algorithms_ask_for_it(monkeypatch):
+    from paper_2607_15810_b200 import binding as B
+    x = torch.ones(3, 256, dtype=torch.bfloat16, device="cuda")
+    w = B.fp8_quantize_weights(torch.ones(1, 48, 256, dtype=torch.bfloat16, device="cuda"))
+    torch.use_deterministic_algorithms(True)
+    try:
+        for native in (B._native, None):
+            monkeypatch.setattr(B, "_native", native)
+            ws = B.fp8_linear(x, w)["workspace"]
+            assert (ws[256:256 + x.numel()] == 255).all()    # three rows are quantized inside the product: nobody writes their codes here
+    finally:
+        torch.use_deterministic_algorithms(False)
