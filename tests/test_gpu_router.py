@@ -290,3 +290,16 @@ def test_ids_and_weights_are_tensors_of_their_own(B, native, monkeypatch):
         f.seek(0)
         a, b = torch.load(f)
         assert a.dtype == torch.int32 and b.dtype == torch.float32 and torch.equal(a, ids) and torch.equal(b, w)
+
+
+def test_sigmoids_below_what_the_exponential_of_the_negated_logit_reaches(B):
+    """exp(-l) is infinite from l = -709.8 on, the sigmoid is above 0 down to -745: the choice is the float64 score's there, too."""
+    l = torch.tensor([[-740.0, -715.0, -730.0, -712.0, -744.0, -720.0, -800.0, -760.0],
+                      [-744.0, -744.0, -713.0, -713.0, -711.0, -760.0, -712.0, -760.0],
+                      [-900.0, -800.0, -760.0, -750.0, -1000.0, -800.0, -760.0, -750.0],
+                      [-1.0, -740.0, -715.0, -730.0, -712.0, -720.0, -699.0, -701.0]])            # (one that float32 tells from the others)
+    for kw in (dict(bias=torch.zeros(8)), dict(n_group=4, topk_group=2, group_top=2), dict(bias=torch.zeros(8), n_group=2, topk_group=1, group_top=2)):
+        ids, _ = B.route_experts(l.cuda(), 3, score="sigmoid", **{k: v.cuda() if torch.is_tensor(v) else v for k, v in kw.items()})
+        for t in range(4):
+            want = R.choose(l[t].double().numpy(), 3, "sigmoid", **{k: v.double().numpy() if torch.is_tensor(v) else v for k, v in kw.items()})
+            assert ids[t].tolist() == want, (t, kw)
