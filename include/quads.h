@@ -424,7 +424,8 @@ quads_status quads_route_experts_backward(const quads_route_args* args /* host *
  *   w_q, w_atoms   as quads_fp8_quantize_weights writes them for one [N, K] weight
  *   out, dx, dw    contiguous, 16-byte aligned, apart from the inputs and from one another (an out that overlaps x is refused); dx
  *                  or dw may be NULL (not computed; x is read for dw only, w_* for dx only)
- *   accumulate     1: dw += (one float32 addition per element), 0: dw =
+ *   accumulate     1: dw +=, in at most one float32 addition per element and 4096 tokens (a longer batch's pieces are added to what is there one
+ *                  after the other, unless clusters of CTAs have added them up before), 0: dw =
  *   workspace      >= quads_fp8_linear_workspace_bytes(T, N, K) / quads_fp8_linear_backward_workspace_bytes(T, N, K), 256-byte aligned;
  *                  never smaller for a larger T
  * N % 16 == 0, K % 16 == 0, both <= 2^20; T < 2^30.  T == 0 does nothing but (accumulate == 0) clear dw.  Every sum runs in a fixed

@@ -648,7 +648,7 @@ def fp8_linear(x, w, workspace=None, out=None):
 def fp8_linear_backward(dy, x=None, w=None, want_dx=True, want_dw=True, dw=None, accumulate=False, workspace=None, dx=None):
     """Gradients of fp8_linear: dy bf16 [T, N], x bf16 [T, K] (needed for dw), w as there (needed for dx).
     Returns dict(dx=bf16 [T, K] = Q(dy) Q(W), dw=float32 [N, K] = Q(dy)^T Q(x), workspace), None for what is not wanted.  `dx`, `dw`: tensors to
-    write to; accumulate: added to the given dw."""
+    write to; accumulate: added to the given dw, in at most one float32 addition per element and 4096 tokens."""
     if _native is not None and want_dx and want_dw and \
             (r := _native.fp8_linear_backward(dy, x, w, dw, accumulate, workspace, dx)) is not None:
         return r

@@ -374,3 +374,23 @@ def test_weights_quantized_where_the_call_in_front_reads_and_from_what_it_writes
         got = B.fp8_quantize_weights(B.fake_quant_activations(ws[0][0], gs=gs)[0][None])
         assert all(torch.equal(got[k], want[k]) for k in want)
         del got
+
+
+# up to 4096 tokens; longer, in clusters, in single CTAs and in pairs
+@pytest.mark.parametrize("T,N,K", [(4096, 144, 272), (4096, 1296, 1296), (9000, 144, 272), (9000, 1296, 1296), (12289, 2064, 2064)])
+def test_a_long_batch_is_added_in_pieces_of_4096_tokens(B, T, N, K):
+    """Whole numbers, exact in every sum of products: what is rounded is the additions to what was there, one per piece or one for all."""
+    g = torch.Generator(device="cuda").manual_seed(T + N)
+    x, dy = (torch.randint(-7, 8, (T, c), generator=g, device="cuda").to(torch.bfloat16) for c in (K, N))
+    start = torch.randn(N, K, generator=g, device="cuda") * 1e4
+    pieces = [(dy[t:t + 4096].double().t() @ x[t:t + 4096].double()).float() for t in range(0, T, 4096)]
+    dw = B.fp8_linear_backward(dy, x, None, want_dx=False)["dw"]
+    assert torch.equal(dw, sum(pieces))
+    for w in (None, B.fp8_quantize_weights(torch.ones(1, N, K, dtype=torch.bfloat16, device="cuda"))):
+        acc = start.clone()
+        B.fp8_linear_backward(dy, x, w, want_dx=w is not None, dw=acc, accumulate=True)
+        one_by_one = start
+        for p in pieces:
+            one_by_one = one_by_one + p
+        assert ((acc == one_by_one) | (acc == start + dw)).all()
+        assert T > 4096 or torch.equal(acc, start + dw)
