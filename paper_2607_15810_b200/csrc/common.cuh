@@ -256,7 +256,7 @@ __device__ __forceinline__ BlockQ quantize_block(const float* v, const QuantCtx&
   const float q0 = __fmul_rn(a, c.r6);
   const float u = __fmaf_rn(__fmaf_rn(-q0, c.d6, a), c.r6, q0);
   BlockQ r;
-  r.sf8 = f32_to_e4m3(u);
+  r.sf8 = f32_to_e4m3(u) & 0x7Fu;          // (inside the table whatever v and the scale hold)
   r.d = __fmul_rn(e4m3_to_f32(r.sf8), c.gs);
   // without the table: the same quotient, one division per block
   const float inv = kLut ? c.inv_lut[r.sf8] : quant_inv_entry(r.sf8, c.gs);

@@ -60,7 +60,7 @@ __device__ __forceinline__ void sum_partial_scores(const float* part, int n_rg, 
   for (int c = threadIdx.x; c < n_ch; c += 256) {
     double t = 0.0;
     for (int l = 0; l < n_sl; ++l) t += red[l * n_ch + c];
-    keys[c] = (unsigned long long)__double_as_longlong(t);   // order-preserving: t >= 0
+    keys[c] = (unsigned long long)__double_as_longlong(fabs(t));   // order-preserving: t >= 0, or a NaN of either sign
   }
 }
 

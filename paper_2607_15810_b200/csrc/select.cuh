@@ -60,7 +60,8 @@ __device__ Selection select_ties(const unsigned long long* sc, const uint32_t* k
 // `nt` threads of a block (128 or more, a multiple of 32; `tid` = 0 .. nt - 1, `sync` is a barrier over them) call it
 // with the same arguments, after a barrier behind the stores to `sc` (shared memory); it returns behind another
 // one.  C is a multiple of 128, at most 16384; `k32` is scratch of C words.  kDoubleKeys: the keys are the bit patterns
-// of non-negative doubles, else integers.
+// of non-negative doubles (a NaN without its sign is the largest: one with it would be above every border that select_ties tries, and
+// more than n_sel channels selected), else integers.
 //   1. A histogram of 1024 bins over the range of the keys' 32-bit images tells which bin the boundary lies in; while
 //      that bin holds many keys it is divided again (outliers stretch the range of the first one).
 //   2. Its keys are listed and ranked among each other by exact key and index.

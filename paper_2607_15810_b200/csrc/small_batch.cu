@@ -329,7 +329,7 @@ front_small_kernel(const SmallFrontArgs p) {
         double s = 0.0;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += red2[w][threadIdx.x];
-        keys[u * 128 + threadIdx.x] = (unsigned long long)__double_as_longlong(s);   // order-preserving: s >= 0
+        keys[u * 128 + threadIdx.x] = (unsigned long long)__double_as_longlong(fabs(s));   // order-preserving: s >= 0, or a NaN of either sign
       }
       __syncthreads();
       for (int i = threadIdx.x; i < 128 * n_cta; i += kSmallThreads) {

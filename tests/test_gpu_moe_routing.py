@@ -278,3 +278,20 @@ def test_native_calls_and_their_python_twins_agree(B, layer, monkeypatch):
     assert r["out"] is out and r["workspace"] is ws
     r = B.fp8_linear_backward(dy, x, q, workspace=ws, dx=dx, dw=dwt)
     assert r["dx"] is dx and r["dw"] is dwt and r["workspace"] is ws
+
+
+@pytest.mark.parametrize("T", [2, 60, 700])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), -float("nan")])
+def test_as_many_channels_as_asked_for_whatever_x_holds(B, layer, T, value):
+    """Scores that are infinite or no numbers, in every channel or in some: the selection has its size and its order."""
+    x, ids = _x(T), _ids(T)
+    w = torch.rand(T, K).cuda()
+    for cols in (slice(0, H), slice(16, 100)):
+        bad = x.clone()
+        bad[::2, cols] = torch.tensor(value, dtype=torch.bfloat16)
+        for gs in (None, torch.tensor([0.002]).cuda()):
+            for n in (1, 100, H - 1):
+                r = B.moe_w4a4_rac(bad, None, *layer["packed"], K, n, 0, layer["a2"], a13_gs=gs, routing=(ids, w), export=True)
+                sel = r["sel13"].tolist()
+                assert len(sel) == n and sel == sorted(set(sel)) and 0 <= sel[0] and sel[-1] < H
+                assert B.moe_async_status(r["workspace"]) == 0
