@@ -292,8 +292,10 @@ typedef struct {
   int32_t expert_lo, expert_count;
   float* out_f32;               /* optional float [T, H]: the call's sum before rounding; `out` may then be NULL */
   /* MoE mode: a routing that is given (quads_route_experts makes such), both or neither: the experts [T, topk] and their weights.
-     router_logits and renormalize are then not read.  A slot whose id is outside 0 .. E-1 contributes nothing; a token that names an
-     expert twice gets it with the sum of the weights. */
+     router_logits and renormalize are then not read.  A slot whose id is outside 0 .. E-1 adds nothing to its token's output; a token that names an
+     expert twice gets it with the sum of the weights.  A token without any expert (a row of padding) has the output 0, but its row of x is part of the
+     batch: the amax that the scale comes from and the channel scores of site 13 count it, as they count every row.  A zero row is as if it were not
+     there; with a13_gs and rac_nsel_13 == 0 it may hold anything, infinities and NaN included. */
   const int32_t* topk_ids_in;
   const float* topk_w_in;
 } quads_moe_args;
@@ -367,7 +369,7 @@ typedef struct {
   uint8_t* hexp;
   void* workspace;
   size_t workspace_bytes;        /* >= quads_moe_fp8_workspace_bytes(T, H, I, E, topk), 256-byte aligned */
-  const int32_t* topk_ids_in;    /* a routing that is given, as in quads_moe_args */
+  const int32_t* topk_ids_in;    /* a routing that is given, as in quads_moe_args; the rows of tokens without any expert may hold anything */
   const float* topk_w_in;
 } quads_moe_fp8_args;
 quads_status quads_moe_fp8_w8a8(const quads_moe_fp8_args* args /* host */, void* cuda_stream);

@@ -239,7 +239,8 @@ def moe_w4a4_rac(x, logits, w13, w2, topk, nsel13, nsel2, a2_gs, a13_gs=None, re
     produced by fake_quant_weights(..., sf_layout=SF_TILED).  Returns dict(out=bf16 [T,H], ...).
 
     logits float32 [T, E]; or None, with routing = (ids int32 [T, topk], weights float32 [T, topk]) as from route_experts: ids outside
-    0 .. E-1 contribute nothing.  n_experts: E then, where it is not the weights' (expert_range)."""
+    0 .. E-1 add nothing to their token's output.  The rows of x count in the scale (without a13_gs) and in the channel selection (nsel13 > 0) all the same, those of
+    tokens without any expert included: zero such rows.  n_experts: E then, where it is not the weights' (expert_range)."""
     if _native is not None and not export and expert_range is None and out_f32 is None and n_experts is None and \
             (r := _native.moe_w4a4_rac(x, logits, w13, w2, topk, nsel13, nsel2, a2_gs, a13_gs, renormalize, workspace, out, routing)) is not None:
         return r
@@ -480,7 +481,8 @@ def moe_fp8_workspace_bytes(T, H, I, E, topk):
 
 
 def moe_fp8_w8a8(x, logits, w13, w2, topk, renormalize=True, export=False, workspace=None, out=None, routing=None):
-    """FP8 W8A8 MoE layer (comparison path).  w13 / w2: dicts from fp8_quantize_weights.  logits, or None and a routing as in moe_w4a4_rac."""
+    """FP8 W8A8 MoE layer (comparison path).  w13 / w2: dicts from fp8_quantize_weights.  logits, or None and a routing as in moe_w4a4_rac (each row has
+    its own scales: those of tokens without any expert may hold anything)."""
     if _native is not None and not export and \
             (r := _native.moe_fp8_w8a8(x, logits, w13, w2, topk, renormalize, workspace, out, routing)) is not None:
         return r

@@ -295,3 +295,50 @@ def test_as_many_channels_as_asked_for_whatever_x_holds(B, layer, T, value):
                 sel = r["sel13"].tolist()
                 assert len(sel) == n and sel == sorted(set(sel)) and 0 <= sel[0] and sel[-1] < H
                 assert B.moe_async_status(r["workspace"]) == 0
+
+
+def _padded(T, seed):
+    """x with the rows of tokens without any expert (every third) left open, and a routing that leaves them and single slots out."""
+    x, ids, w = _x(T, seed), _ids(T, seed), torch.rand(T, K, generator=torch.Generator().manual_seed(seed)).cuda()
+    empty = torch.arange(T).cuda() % 3 == 2
+    ids[empty] = -1
+    ids[::4, 1] = E
+    w[(ids < 0) | (ids >= E)] = float("nan")               # (the weights of such slots are not read, or not used)
+    return x, (ids, w), empty
+
+
+@pytest.mark.parametrize("T", [3, 60, 600, 3000])
+def test_rows_without_an_expert_count_in_the_scale_and_the_selection(B, layer, T):
+    """The layer's x is its whole batch, tokens that no expert takes included: their rows are zeroed, and are then as if they were not there, or the scale is
+    given and nothing selected."""
+    x, rt, empty = _padded(T, 51)
+    n = H // 2
+    run = lambda x, n13, gs: B.moe_w4a4_rac(x, None, *layer["packed"], K, n13, I // 2, layer["a2"], a13_gs=gs, routing=rt, export=True)
+    real = x[~empty].contiguous()
+    zeroed = x.masked_fill(empty[:, None], 0.0)
+    r = run(zeroed, n, None)
+    assert r["a13_gs"].item() == np.float32(np.float32(real.abs().max().item()) / np.float32(2688.0))
+    scores = B.rac_channel_scores(real)
+    # float32 sums over some rows each, then float64: off by a step (2^-23) of the sum for each of the T rows at most
+    chosen = torch.zeros(H, dtype=torch.bool).cuda()
+    chosen[r["sel13"].long()] = True
+    assert chosen.sum() == n and scores[chosen].min() * (1 + T * 2.0 ** -22) >= scores[~chosen].max()
+    loud = x.clone()
+    loud[empty] = 1e4
+    assert run(loud, n, None)["a13_gs"].item() == np.float32(np.float32(torch.tensor(1e4, dtype=torch.bfloat16).item()) / np.float32(2688.0))
+    gs = r["a13_gs"].clone()
+    want = run(zeroed, 0, gs)["out"]
+    assert (want[empty] == 0).all()
+    for v in (1e30, float("nan"), float("inf")):
+        got = run(x.masked_fill(empty[:, None], v), 0, gs)
+        assert torch.equal(got["out"], want) and B.moe_async_status(got["workspace"]) == 0
+
+
+@pytest.mark.parametrize("T", [3, 60, 600, 3000])
+def test_rows_without_an_expert_are_of_no_account_in_the_fp8_layer(B, layer, T):
+    x, rt, empty = _padded(T, 52)
+    want = B.moe_fp8_w8a8(x, None, *layer["fp8"], K, routing=rt)["out"]
+    assert (want[empty] == 0).all()
+    for v in (0.0, 1e30, float("nan"), -float("inf")):
+        got = B.moe_fp8_w8a8(x.masked_fill(empty[:, None], v), None, *layer["fp8"], K, routing=rt)
+        assert torch.equal(got["out"], want) and B.moe_async_status(got["workspace"]) == 0
