@@ -11,6 +11,10 @@
  *     Workspaces must be 256-byte aligned.
  *   - Work is enqueued on `cuda_stream` (a cudaStream_t passed as void*; NULL =
  *     the legacy default stream) and the call returns without synchronising.
+ *   - The args structs grow at their end and hold no size: zero-initialise them, and
+ *     rebuild callers with the header of the library that they load.  From a caller built with
+ *     a former one the library reads the new fields behind its struct.  (The last ones:
+ *     topk_ids_in and topk_w_in of quads_moe_args and quads_moe_fp8_args.)
  *   - Argument errors are detected on the host and returned before anything is
  *     launched.  A CUDA launch error is returned as QUADS_ERR_CUDA.  A device
  *     wait that ran out of its iteration budget is recorded in the workspace and

@@ -84,3 +84,23 @@ def test_binding_loads_where_torch_has_no_cuda():
             "from paper_2607_15810_b200 import binding as B\n"
             "assert B.sf_tiled_bytes(128, 64) == 512\n")
     subprocess.run([sys.executable, "-c", code], check=True, cwd=ROOT)
+
+
+def test_the_bindings_structs_are_the_headers(lib, tmp_path):
+    """Sizes and offsets of every field, as a C compiler lays the header's structs out."""
+    from paper_2607_15810_b200 import binding as B
+    structs = {"quads_moe_args": B.MoEArgs, "quads_moe_fp8_args": B.MoEFp8Args, "quads_route_args": B.RouteArgs}
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "quads.h")).read(), flags=re.S)
+    assert set(re.findall(r"\}\s*(quads_\w+_args);", text)) == set(structs)
+    lines, want = [], []
+    for name, cls in structs.items():
+        lines.append('printf("%%zu\\n", sizeof(%s));' % name)
+        want.append(C.sizeof(cls))
+        for field, _ in cls._fields_:
+            lines.append('printf("%%zu\\n", offsetof(%s, %s));' % (name, field))
+            want.append(getattr(cls, field).offset)
+    source = tmp_path / "layout.c"
+    source.write_text('#include <stdio.h>\n#include "quads.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0;\n}\n")
+    subprocess.run(["gcc", "-I" + os.path.join(ROOT, "include"), str(source), "-o", str(tmp_path / "layout")], check=True)
+    out = subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout
+    assert [int(v) for v in out.split()] == want
