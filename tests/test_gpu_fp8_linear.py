@@ -394,3 +394,17 @@ def test_a_long_batch_is_added_in_pieces_of_4096_tokens(B, T, N, K):
             one_by_one = one_by_one + p
         assert ((acc == one_by_one) | (acc == start + dw)).all()
         assert T > 4096 or torch.equal(acc, start + dw)
+
+
+# in single CTAs, in clusters, in pairs
+@pytest.mark.parametrize("T,N,K", [(16384, 1280, 1280), (16384, 144, 272), (16384, 1664, 1680), (9000, 1296, 1296)])
+def test_weight_gradients_of_long_batches_keep_float32s_precision(B, T, N, K):
+    """What leaving the tensor core every 4096 tokens is for: its additions cut off, and the relative error (2-norm) of terms of like magnitude grows
+    with their number: 6.0e-8 at 1024 tokens, 2.2e-7 at 4096 and, in one piece, 4.8e-7 at 8192, 5.3e-7 at 9000, 1.16e-6 at 16384.  The sum of
+    pieces of 4096 has their 2.2e-7, and the three additions of four of them are off by half a step each: 2.2e-7 + 3 x 2^-24."""
+    g = torch.Generator().manual_seed(T + N)
+    x, dy = (torch.randn(T, c, generator=g).to(torch.bfloat16) for c in (K, N))
+    dw = B.fp8_linear_backward(dy.cuda(), x.cuda(), None, want_dx=False)["dw"]
+    rows = torch.randperm(N, generator=g)[:64]
+    want, _ = L.grad_weight(_f32(dy[:, rows]), _f32(x))
+    assert np.linalg.norm(_f32(dw[rows.cuda()]) - want) <= (2.2e-7 + 3 * 2.0 ** -24) * np.linalg.norm(want)
