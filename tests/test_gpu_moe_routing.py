@@ -342,3 +342,24 @@ def test_rows_without_an_expert_are_of_no_account_in_the_fp8_layer(B, layer, T):
     for v in (0.0, 1e30, float("nan"), -float("inf")):
         got = B.moe_fp8_w8a8(x.masked_fill(empty[:, None], v), None, *layer["fp8"], K, routing=rt)
         assert torch.equal(got["out"], want) and B.moe_async_status(got["workspace"]) == 0
+
+
+# the layer's three routing kernels (512 and 513 tokens apart), weights renormalised or not
+@pytest.mark.parametrize("T", [1, 61, 500, 513, 3000])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_the_softmax_routers_choice_given_to_the_layers_is_their_own(B, layer, T, renorm):
+    lg = torch.randn(T, E, generator=torch.Generator().manual_seed(T + 7)).cuda()
+    lg[::3, 4] = lg[::3, 9]                                # equal logits
+    x, rt = _x(T, 61), B.route_experts(lg, K, renormalize=renorm)
+    own = B.moe_w4a4_rac(x, lg, *layer["packed"], K, H // 2, I // 2, layer["a2"], renormalize=renorm, export=True)
+    given = B.moe_w4a4_rac(x, None, *layer["packed"], K, H // 2, I // 2, layer["a2"], routing=rt, export=True)
+    for k in ("ids", "offsets", "perm", "sel13", "sel2", "h", "hq"):
+        assert torch.equal(given[k], own[k]), k
+    # either weight: exp within 2 ulp in numerator and denominator (8 half steps), its argument (2 x 8 of them: |l - m| <= 8), sums of up to 16
+    # terms (16), one or two divisions (4 each)
+    assert ((given["weights"] - own["weights"]).abs() <= 2 * 48 * 2.0 ** -24 * own["weights"]).all()
+    fp8 = [B.moe_fp8_w8a8(x, *a, *layer["fp8"], K, renormalize=renorm, routing=r)["out"] for a, r in (((lg,), None), ((None,), rt))]
+    for a, b in ((own["out"], given["out"]), fp8):
+        # K terms with weights that far apart (bounded by the terms' sum: 4 x the largest output of the row), one rounding to bf16 of either
+        a, b = a.double(), b.double()
+        assert ((a - b).abs() <= 2 * 2.0 ** -8 * a.abs() + 128 * 2.0 ** -24 * 4 * a.abs().amax(1, keepdim=True)).all()

@@ -99,3 +99,53 @@ def test_expert_parallel_helper_partitions_the_experts_and_sums_the_partials(tmp
     out = json.loads([ln for ln in r.stdout.splitlines() if ln.startswith("{")][0])
     assert out["ranges"] == [[0, 5], [5, 10]] and out["value"] == float(sum(range(10)))
     assert out["shape"] == [6, 8] and out["dtype"] == "torch.bfloat16"
+
+
+EP_ROUTING_WORKER = r"""
+import os, sys, json
+sys.path.insert(0, %r)
+import torch
+from paper_2607_15810_b200 import dist_util as D
+from paper_2607_15810_b200 import ep
+world, rank = D.init("gloo")
+E, T, H, K = 10, 6, 8, 3
+
+
+class FakeBinding:
+    # stands in for the CUDA library on CPU: experts multiply by their id + 1, slots outside the rank's experts add nothing
+    def moe_w4a4_rac(self, x, logits, w13, w2, topk, n13, n2, a2, expert_range=None, out_f32=None, routing=None, n_experts=None):
+        lo, hi = expert_range
+        assert logits is None and n_experts == E and w13["q"].shape[0] == hi - lo and w2["q"].shape[0] == hi - lo
+        ids, w = routing
+        assert ids.shape == w.shape == (T, topk)
+        mine = (ids >= lo) & (ids < hi)
+        out_f32.copy_((x[:, None] * (w * (ids + 1) * mine)[:, :, None]).sum(1))
+
+g = torch.Generator().manual_seed(1)
+x, w = torch.randint(-8, 9, (T, H), generator=g).float(), torch.randint(1, 4, (T, K), generator=g).float()
+ids = torch.stack([torch.randperm(E, generator=g)[:K] for _ in range(T)]).to(torch.int32)
+ids[2], ids[4, 1] = -1, E
+weights = {"q": torch.zeros(E, 2), "sf": torch.zeros(E, 2), "gs": torch.zeros(E)}
+lo, hi = ep.expert_range(rank, world, E)
+shards = ep.shard_weights(weights, lo, hi), ep.shard_weights(weights, lo, hi)
+out = ep.moe_w4a4_rac_expert_parallel(FakeBinding(), x, None, *shards, K, 0, 0, None, rank, world, routing=(ids, w), n_experts=E)
+there = (ids >= 0) & (ids < E)
+want = (x[:, None] * (w * (ids + 1) * there)[:, :, None]).sum(1).to(torch.bfloat16)
+try:
+    ep.moe_w4a4_rac_expert_parallel(FakeBinding(), x, None, *shards, K, 0, 0, None, rank, world, routing=(ids, w))
+    refused = False
+except KeyError:                                       # how many experts there are is not the shard's to say
+    refused = True
+print(json.dumps({"rank": rank, "equal": torch.equal(out, want), "empty": bool((out[2] == 0).all()), "refused": refused}))
+D.shutdown()
+"""
+
+
+def test_expert_parallel_helper_with_a_routing_that_is_given(tmp_path):
+    """logits None: both ranks get the whole routing, each adds its own experts' slots, the all-reduce has every slot once."""
+    script = tmp_path / "ep_routing_worker.py"
+    script.write_text(EP_ROUTING_WORKER % ROOT)
+    r = _torchrun([str(script)], 240)
+    assert r.returncode == 0, r.stderr[-2000:]
+    out = sorted((json.loads(ln) for ln in r.stdout.splitlines() if ln.startswith("{")), key=lambda d: d["rank"])
+    assert out == [{"rank": i, "equal": True, "empty": True, "refused": True} for i in range(2)]
