@@ -64,3 +64,45 @@ def test_long_predecessor_is_not_a_timeout(monkeypatch):
         B.lib.quads_debug_set_quantize_wait(0, 0)
     assert bool(torch.isnan(gs).all()) and start.elapsed_time(end) > 2200.0          # (the predecessor did take that long)
     assert status == 0 and torch.equal(out, want)
+
+
+# rows quantized inside the product; by rows; in tiles of 128 x 128, with pairs behind; gradients of small tensors and of larger ones
+@pytest.mark.parametrize("T,K,N,backward", [(3, 512, 512, False), (61, 512, 1040, False), (4096, 4096, 2064, False), (61, 512, 1040, True),
+                                            (2100, 2048, 2064, True)])
+def test_projections_report_and_clear_the_status_word(T, K, N, backward):
+    """What a wait that was given up leaves there is read by the status call, and the next call on the workspace clears it."""
+    from paper_2607_15810_b200 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x, dy, w = (torch.randn(*s, device="cuda", generator=g).to(torch.bfloat16) for s in ((T, K), (T, N), (1, N, K)))
+    q = B.fp8_quantize_weights(w)
+    run = (lambda **kw: B.fp8_linear_backward(dy, x, q, **kw)) if backward else (lambda **kw: B.fp8_linear(x, q, **kw))
+    want = run()
+    ws = want["workspace"].clone().fill_(0xFA)
+    ws[:32].view(torch.int32)[3] = -6                        # QUADS_ERR_TIMEOUT
+    assert B.moe_async_status(ws) == -6
+    got = run(workspace=ws)
+    assert B.moe_async_status(ws) == 0
+    for k in ("dx", "dw") if backward else ("out",):
+        assert torch.equal(got[k], want[k])
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T", [7, 600])
+def test_layers_with_a_given_routing_clear_the_status_word(T, fp8):
+    from paper_2607_15810_b200 import binding as B
+    E, H, I, K = 8, 256, 128, 2
+    g = torch.Generator(device="cuda").manual_seed(T)
+    bf = lambda *s: (torch.randn(*s, device="cuda", generator=g) * 0.1).to(torch.bfloat16)
+    rt = B.route_experts(torch.randn(T, E, device="cuda", generator=g), K)
+    if fp8:
+        w = [B.fp8_quantize_weights(bf(*s)) for s in ((E, 2 * I, H), (E, H, I))]
+        ws, run = B.moe_fp8_workspace_bytes(T, H, I, E, K), lambda ws: B.moe_fp8_w8a8(bf(T, H), None, *w, K, workspace=ws, routing=rt)
+    else:
+        w = [B.fake_quant_weights(bf(*s), want_fq=False, sf_layout=B.SF_TILED) for s in ((E, 2 * I, H), (E, H, I))]
+        a2 = torch.tensor([0.01], device="cuda")
+        ws, run = B.moe_workspace_bytes(T, H, I, E, K), lambda ws: B.moe_w4a4_rac(bf(T, H), None, *w, K, 64, 64, a2, workspace=ws, routing=rt)
+    ws = torch.full((ws,), 0xFA, dtype=torch.uint8, device="cuda")
+    ws[:32].view(torch.int32)[3] = -6
+    assert B.moe_async_status(ws) == -6
+    run(ws)
+    assert B.moe_async_status(ws) == 0
