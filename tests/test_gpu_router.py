@@ -303,3 +303,15 @@ def test_sigmoids_below_what_the_exponential_of_the_negated_logit_reaches(B):
         for t in range(4):
             want = R.choose(l[t].double().numpy(), 3, "sigmoid", **{k: v.double().numpy() if torch.is_tensor(v) else v for k, v in kw.items()})
             assert ids[t].tolist() == want, (t, kw)
+
+
+def test_weights_of_equal_logits_are_rounded_once(B):
+    """Scores of 1 among k or E of them: numerator and sum are exact, and the quotient by an approximate reciprocal and a Newton step is off by some 2^-46 of itself
+    before it is rounded; no 1 / n with n up to 256 is within 2^-32 of itself of the middle between two float32s."""
+    for n in range(1, 257):
+        want = torch.tensor(1.0 / n, dtype=torch.float64).float().item()
+        l = torch.zeros(2, n).cuda()
+        assert (B.route_experts(l, 1, renormalize=False)[1] == want).all(), n
+        if n <= 16:
+            assert (B.route_experts(torch.zeros(2, 40).cuda(), n)[1] == want).all(), n
+            assert (B.route_experts(torch.zeros(2, 40).cuda(), n, score="sigmoid")[1] == want).all(), n
