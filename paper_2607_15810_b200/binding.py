@@ -245,6 +245,7 @@ def moe_w4a4_rac(x, logits, w13, w2, topk, nsel13, nsel2, a2_gs, a13_gs=None, re
             (r := _native.moe_w4a4_rac(x, logits, w13, w2, topk, nsel13, nsel2, a2_gs, a13_gs, renormalize, workspace, out, routing)) is not None:
         return r
     assert (logits is None) != (routing is None), "logits or a routing"
+    assert _here(x, logits, w13["q"], w2["q"]), "on the current device, whose stream takes the launch"
     assert n_experts is None or (routing is not None and expert_range is not None), "n_experts goes with a routing and expert_range"
     T, H = x.shape
     E = logits.shape[1] if routing is None else n_experts if n_experts is not None else w13["q"].shape[0]
@@ -466,7 +467,7 @@ lib.quads_moe_fp8_workspace_bytes.argtypes = [_i32] * 5
 
 def fp8_quantize_weights(w):
     """w: bf16 CUDA [n, N, K], N and K multiples of 16 -> dict(q u8 [n, N, K], exps u8 [n, ceil(N/128), ceil(K/128)], atoms u8 [.., 512])."""
-    assert w.dtype == torch.bfloat16 and w.is_cuda and w.dim() == 3 and w.is_contiguous()
+    assert w.dtype == torch.bfloat16 and w.is_cuda and w.dim() == 3 and w.is_contiguous() and _here(w)
     n, N, K = w.shape
     dev = w.device
     q = torch.empty(n, N, K, dtype=torch.uint8, device=dev)
@@ -487,6 +488,7 @@ def moe_fp8_w8a8(x, logits, w13, w2, topk, renormalize=True, export=False, works
             (r := _native.moe_fp8_w8a8(x, logits, w13, w2, topk, renormalize, workspace, out, routing)) is not None:
         return r
     assert (logits is None) != (routing is None), "logits or a routing"
+    assert _here(x, logits, w13["q"], w2["q"]), "on the current device, whose stream takes the launch"
     T, H = x.shape
     E = logits.shape[1] if routing is None else w13["q"].shape[0]
     I = w2["q"].shape[2]

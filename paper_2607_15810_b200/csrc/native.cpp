@@ -212,7 +212,7 @@ bool read_routing(PyObject* logits, PyObject* routing, const at::Tensor* q, int6
   *r = Routing{};
   if (routing == Py_None) {
     const at::Tensor* lg = cuda_tensor(logits);
-    if (!lg || lg->dim() < 2 || lg->size(1) > INT32_MAX) return false;
+    if (!lg || lg->dim() < 2 || lg->size(1) > INT32_MAX || !is_here(*lg)) return false;
     r->E = (int32_t)lg->size(1);
     r->logits = (const float*)ptr(lg);
     return true;
@@ -238,7 +238,9 @@ PyObject* moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *q1 = entry(a[2], s_q), *f1 = entry(a[2], s_sf), *g1 = entry(a[2], s_gs);
   const at::Tensor *q2 = entry(a[3], s_q), *f2 = entry(a[3], s_sf), *g2 = entry(a[3], s_gs);
   Routing rt;
-  if (!q1 || !f1 || !g1 || !q2 || !f2 || !g2 || q2->dim() < 3 || q2->size(2) > INT32_MAX / 2 || !read_routing(a[1], a[12], q1, m.T, m.topk, &rt)) Py_RETURN_NONE;
+  if (!q1 || !f1 || !g1 || !q2 || !f2 || !g2 || q2->dim() < 3 || q2->size(2) > INT32_MAX / 2 || !read_routing(a[1], a[12], q1, m.T, m.topk, &rt) ||
+      !is_here(*x) || !is_here(*q1) || !is_here(*q2))
+    Py_RETURN_NONE;
   const int renorm = PyObject_IsTrue(a[9]);
   if (renorm < 0) return nullptr;
   m.E = rt.E;
@@ -270,7 +272,9 @@ PyObject* moe_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   const at::Tensor *q1 = entry(a[2], s_q), *t1 = entry(a[2], s_atoms), *q2 = entry(a[3], s_q), *t2 = entry(a[3], s_atoms);
   Routing rt;
-  if (!q1 || !t1 || !q2 || !t2 || q2->dim() < 3 || q2->size(2) > INT32_MAX || !read_routing(a[1], a[8], q1, x->size(0), m.topk, &rt)) Py_RETURN_NONE;
+  if (!q1 || !t1 || !q2 || !t2 || q2->dim() < 3 || q2->size(2) > INT32_MAX || !read_routing(a[1], a[8], q1, x->size(0), m.topk, &rt) || !is_here(*x) ||
+      !is_here(*q1) || !is_here(*q2))
+    Py_RETURN_NONE;
   const int renorm = PyObject_IsTrue(a[5]);
   if (renorm < 0) return nullptr;
   m.T = (int32_t)x->size(0); m.H = (int32_t)x->size(1); m.I = (int32_t)q2->size(2); m.E = rt.E;

@@ -363,3 +363,19 @@ def test_the_softmax_routers_choice_given_to_the_layers_is_their_own(B, layer, T
         # K terms with weights that far apart (bounded by the terms' sum: 4 x the largest output of the row), one rounding to bf16 of either
         a, b = a.double(), b.double()
         assert ((a - b).abs() <= 2 * 2.0 ** -8 * a.abs() + 128 * 2.0 ** -24 * 4 * a.abs().amax(1, keepdim=True)).all()
+
+
+def test_tensors_of_another_device_are_refused(B, layer, monkeypatch):
+    """The launch goes to the current device's stream; here the tensors' device is the first and the second is called the current one."""
+    x, lg, rt = _x(4), torch.randn(4, E).cuda(), (_ids(4), torch.rand(4, K).cuda())
+    w = torch.zeros(1, 32, 64, dtype=torch.bfloat16).cuda()
+    q = B.fp8_quantize_weights(w)
+    monkeypatch.setattr(B, "_native", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in _calls(B, layer).values():
+        for a in ((lg, None), (None, rt)):
+            with pytest.raises(AssertionError):
+                call(x, *a)
+    for f in (lambda: B.fp8_quantize_weights(w), lambda: B.fp8_linear(w[0, :4], q), lambda: B.route_experts(lg, 2), lambda: B.route_experts_backward(lg, *rt)):
+        with pytest.raises(AssertionError):
+            f()
