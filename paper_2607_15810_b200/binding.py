@@ -522,6 +522,8 @@ def moe_fp8_w8a8(x, logits, w13, w2, topk, renormalize=True, export=False, works
 
 
 # ---------------------------------------------------------------- the router by itself, the dense FP8 projection
+# No call records an autograd graph: results are detached, also those of tensors that require gradients; a trainer calls the *_backward functions from
+# an autograd function of its own.
 class RouteArgs(C.Structure):
     _fields_ = [
         ("T", _i32), ("E", _i32), ("topk", _i32), ("score", _i32), ("n_group", _i32), ("topk_group", _i32), ("group_top", _i32),
@@ -573,7 +575,8 @@ def route_experts(logits, topk, score="softmax", bias=None, n_group=1, topk_grou
     score "softmax" or "sigmoid"; experts are chosen by score + bias (float32 [E]), with n_group > 1 among the topk_group groups of
     E / n_group consecutive experts whose group_top (1 or 2) best add up to most; ties to the lower id.  Weights: scale * score,
     renormalised over the chosen ones.  A logit (or a bias) of -inf takes its expert out; a token's slots that stay empty hold id -1 and weight 0.
-    `out`: (ids, weights) to write to.  The result is what moe_w4a4_rac and moe_fp8_w8a8 take as `routing`."""
+    `out`: (ids, weights) to write to.  The result is what moe_w4a4_rac and moe_fp8_w8a8 take as `routing`; detached: the weights' gradient is
+    route_experts_backward's."""
     if _native is not None and out is None and \
             (r := _native.route_experts(logits, topk, score, bias, n_group, topk_group, group_top, renormalize, scale)) is not None:
         return r
@@ -634,7 +637,8 @@ def _bf16_rows(t, cols):
 
 def fp8_linear(x, w, workspace=None, out=None):
     """FP8 projection: x bf16 [T, K] (row stride allowed), quantized online per (row, 128 channels); w: one weight [N, K] as from
-    fp8_quantize_weights.  N and K multiples of 16; `out` apart from x.  Returns dict(out=bf16 [T, N], workspace)."""
+    fp8_quantize_weights.  N and K multiples of 16; `out` apart from x.  Returns dict(out=bf16 [T, N], workspace), detached: the gradients are
+    fp8_linear_backward's."""
     if _native is not None and (r := _native.fp8_linear(x, w, workspace, out)) is not None:
         return r
     q, atoms, N, K = _fp8_weight(w)

@@ -333,7 +333,8 @@ __device__ __forceinline__ void tmem_ld32_bits(uint32_t taddr, uint32_t* r) {
 // ---------------------------------------------------------------------------
 // Large products: persistent pairs of CTAs, 256 x 256 or 256 x 192 tiles (cta_group::2), each CTA with its own 128 rows of A and half of B's
 // -- 32 or 28 KB a stage and 128 of K, six or seven stages.  One float32 accumulator of 256 columns (two do not fit beside the scales), drained
-// by sixteen warps into registers at once.
+// by sixteen warps into registers at once.  (96 registers a thread leave the form of 256 columns a stack of 16 bytes: 24 bytes of spill stores, 64 of
+// loads.  The form of 192 columns has none.)
 // ---------------------------------------------------------------------------
 template <int kN>
 struct PCfg {

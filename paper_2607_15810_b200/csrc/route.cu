@@ -157,8 +157,8 @@ constexpr float kSmallSigmoid = -700.f;
 
 // The choice in float64, for the tokens whose float32 scores lie too near to one another: slow and exact.  Lane s < topk gets slot s.
 // keys [NJ][32], a column per lane: in shared memory and loops, because in registers, or in a function that is called, they give the
-// kernel a stack, and the launch of one that has any takes 0.4 us longer.  (Unrolled so far as that leaves none: 16384 tokens, all of them near,
-// 76 us with no unrolling.)
+// kernel a stack, and the launch of one that has any takes 0.4 us longer.  (Unrolled so far as that leaves none: 16384 tokens, all of them near, 68 us,
+// 76 with no unrolling.)
 template <int NJ, bool kBf16>
 __device__ __forceinline__ int choose_exact(const RouterParams& p, int64_t t, uint64_t* keys) {
   const int lane = threadIdx.x & 31;
@@ -340,11 +340,12 @@ __device__ __forceinline__ float ex2_approx(float x) { float r; asm("ex2.approx.
 // smax 2^-19 down to smax = 2^-9 (|l| < 6.3).  Softmax: the same for the terms, 2^-20 for the sum of 256: d = smax 2^-19.  Where two
 // neighbours in rank lie nearer than twice that, those gathered are ranked in float64; where two groups do, or smax is less, the
 // token is chosen in float64 from the start.
-// Bound by instruction issue at many tokens (some 900 a token with sigmoid, bias and groups, 500 by logits), by the latency of the chain at
-// few.  Replayed from a graph: 16384 tokens of 256 experts, sigmoid, bias and groups 19.1 us (with the float64 parts as functions that are
-// called 21 to 23; all tokens in float64 68), softmax 10.2 (keys of 64 bits, a maximum of all of them per slot: 30.5); one token 2.9 and 2.0.
-// Measured on the form with calls: five CTAs on an SM 22.9 against 20.7, six 23.6; two tokens to a warp, 16 lanes each, shuffles in place of the
-// warp's reduction, 256 experts 28.4 and 14.9, 128 experts 10.2 and 6.5 against 11.0 and 6.9.
+// Bound by the latency of the chain of a warp's reductions and votes, one token at a time in a warp: at many tokens 52 to 54 % of the issue slots are taken
+// (some 900 instructions a token with sigmoid, bias and groups, 480 by logits), and 16384 tokens are three and a half rounds of them.  Replayed from a graph: 16384
+// tokens of 256 experts, sigmoid, bias and groups 19.2 to 23.7 us with the draw (23.4 with a token chosen in float64 in the last round; with the float64 parts as
+// functions that are called 21 to 23; all tokens in float64 75), softmax 10.1 (keys of 64 bits, a maximum of all of them per slot: 30.5); one token 3.0 and
+// 2.0.  Measured on the form with calls: five CTAs on an SM 22.9 against 20.7, six 23.6; two tokens to a warp, 16 lanes each, shuffles in place of the
+// warp's reduction, 256 experts 28.4 and 14.9, 128 experts 10.2 and 6.5 against 11.0 and 6.9 (not taken for few experts alone: not measured on the present form).
 template <int NJ, bool kBf16>
 __global__ void __launch_bounds__(kRouterWarps * 32, NJ <= 8 ? 4 : 2)
 route_experts_kernel(const RouterParams p) {
