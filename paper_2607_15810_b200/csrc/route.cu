@@ -341,9 +341,9 @@ __device__ __forceinline__ float ex2_approx(float x) { float r; asm("ex2.approx.
 // neighbours in rank lie nearer than twice that, those gathered are ranked in float64; where two groups do, or smax is less, the
 // token is chosen in float64 from the start.
 // Bound by the latency of the chain of a warp's reductions and votes, one token at a time in a warp: at many tokens 52 to 54 % of the issue slots are taken
-// (some 900 instructions a token with sigmoid, bias and groups, 480 by logits), and 16384 tokens are three and a half rounds of them.  Replayed from a graph: 16384
-// tokens of 256 experts, sigmoid, bias and groups 19.2 to 23.7 us with the draw (23.4 with a token chosen in float64 in the last round; with the float64 parts as
-// functions that are called 21 to 23; all tokens in float64 75), softmax 10.1 (keys of 64 bits, a maximum of all of them per slot: 30.5); one token 3.0 and
+// (some 900 instructions a token with sigmoid, bias and groups, 480 by logits), and of 16384 tokens a warp takes three or four.  Replayed from a graph: 16384
+// tokens of 256 experts, sigmoid, bias and groups 19.2 to 23.7 us (more where one of the tokens that the warps take last is chosen in float64; all tokens
+// in float64 75), softmax 10.1 (keys of 64 bits, a maximum of all of them per slot: 30.5); one token 3.0 and
 // 2.0.  Measured on the form with calls: five CTAs on an SM 22.9 against 20.7, six 23.6; two tokens to a warp, 16 lanes each, shuffles in place of the
 // warp's reduction, 256 experts 28.4 and 14.9, 128 experts 10.2 and 6.5 against 11.0 and 6.9 (not taken for few experts alone: not measured on the present form).
 template <int NJ, bool kBf16>
